@@ -934,9 +934,11 @@ __global__ void __launch_bounds__(256, 2) attend_tile_kernel(AttendArgs a, Atten
     mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
     // The reference follows a row's maximum only when that has outgrown it 2^8 times (a probability is then at most
     // 256 and rounded like any other): else one of 32 rows raises its own on most pages and every sum is scaled
-    // (4096 rows behind 4000: 811 -> 781 us).
-    if (!__all(mx <= mrun + slack)) {
-      const float mnew = fmaxf(mrun, mx);
+    // (4096 rows behind 4000: 811 -> 781 us).  Each row goes by its own scores, or its rounding would depend on
+    // what the others see.
+    const bool within = mx <= mrun + slack;
+    if (!__all(within)) {
+      const float mnew = within ? mrun : mx;
       const float alpha = mnew == mrun ? 1.f : __builtin_amdgcn_exp2f((mrun - mnew) * c);
       mrun = mnew;
       lrun *= alpha;
