@@ -48,10 +48,11 @@ struct AttendPlan {
   float* o;     // [slots][tile][hd] sums of p v
   float* ml;    // [slots][tile][2] maximum (log2 units), sum of p
   // cap * tanh(x), x = s * cap_ratio, is in log2 units s * poly(x^2) up to |s| = cap_limit, half of the cap: tanh(x) / x
-  // in x^2 to 5.5e-7, fitted over [0, 1/4], times the scale.  The tile kernel takes s * fold(s^2) for a whole page, up to
-  // |s| = fold_limit: powers of the ratio folded in spare a multiplication (capped scores, 256 positions of window: 53 ->
-  // 51 us); where they would leave fp32's range no score is below that limit.
-  float cap_ratio, cap_limit, cap_poly[4], fold_limit, cap_fold[4];
+  // in x^2 to 5.5e-7, fitted over [0, 1/4], times the scale.  The powers of the ratio are folded into the coefficients,
+  // poly then takes s^2 (poly_ratio 1), but where they would leave fp32's range (poly_ratio is the ratio).  A page whose
+  // scores all lie below fold_limit, the limit where they are folded, takes the polynomial without that multiplication
+  // (256 positions of window: 53 -> 51 us); a score gets the same bits on either way.
+  float cap_ratio, cap_limit, poly_ratio, cap_poly[4], fold_limit;
   TileCut* how; // written by the tile kernel for the merge
   int* parts;   // stream kernel: arrivals of a cut chain's parts [target][n_kv], zero between calls; NULL:
                 // the merge kernel joins them
@@ -275,7 +276,7 @@ template <typename T, int MOD> LSV_DEV float capped_of(const AttendArgs& a, cons
     const float cap = a.softcap * kLog2e;
     const float e = __builtin_amdgcn_exp2f(s * (2.f * kLog2e * pl.cap_ratio));
     const float big = fmaf(-2.f * cap, __builtin_amdgcn_rcpf(e + 1.f), cap);
-    const float x = s * pl.cap_ratio;
+    const float x = s * pl.poly_ratio;
     return fabsf(s) <= pl.cap_limit ? cap_poly(pl.cap_poly, s, x * x) : big;
   }
 }
@@ -907,7 +908,7 @@ __global__ void __launch_bounds__(256, 2) attend_tile_kernel(AttendArgs a, Atten
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) sc[kb][r] = cap_poly(pl.cap_fold, sc[kb][r], sc[kb][r] * sc[kb][r]);
+          for (int r = 0; r < 16; ++r) sc[kb][r] = cap_poly(pl.cap_poly, sc[kb][r], sc[kb][r] * sc[kb][r]);
       }
     }
     if (MOD && !(MOD == kCapped && small)) {
@@ -1230,14 +1231,13 @@ int launch_attend(int dtype, const AttendArgs& a, void* ws, hipStream_t st) {
   if (a.softcap > 0.f) {
     const double fit[4] = {0.999999456, -0.33326318, 0.131902968, -0.0444022301};
     const double ratio = (double)a.scale / a.softcap;
-    for (int i = 0; i < 4; ++i) {
-      pl.cap_poly[i] = (float)(fit[i] * a.scale * kLog2e);
-      pl.cap_fold[i] = (float)(fit[i] * a.scale * kLog2e * pow(ratio, 2 * i));
-    }
-    pl.cap_ratio = (float)ratio;
-    pl.cap_limit = (float)fmin(0.5 / fabs(ratio), 1e30);  // infinities are above it
     auto near_one = [](double x, double far) { return fabs(x) >= 1.0 / far && fabs(x) <= far; };
-    pl.fold_limit = near_one(ratio, 1e5) && near_one(a.scale, 1e7) ? pl.cap_limit : -1.f;
+    const bool fold = near_one(ratio, 1e5) && near_one(a.scale, 1e7);
+    for (int i = 0; i < 4; ++i) pl.cap_poly[i] = (float)(fit[i] * a.scale * kLog2e * (fold ? pow(ratio, 2 * i) : 1.0));
+    pl.cap_ratio = (float)ratio;
+    pl.poly_ratio = fold ? 1.f : pl.cap_ratio;
+    pl.cap_limit = (float)fmin(0.5 / fabs(ratio), 1e30);  // infinities are above it
+    pl.fold_limit = fold ? pl.cap_limit : -1.f;
   }
   pl.how = (TileCut*)ws;
   pl.parts = p.join ? (int*)((char*)ws + 256) : nullptr;

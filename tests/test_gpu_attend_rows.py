@@ -30,7 +30,7 @@ def rising(seed, dtype, hd, C, rows, **opts):
 
 
 BLOCKS = [([300], [2]), ([300, 70], [40, 90]), ([1000], [64])]
-SCORES = [{}, dict(slopes=[0.01] * 8)]
+SCORES = [{}, dict(slopes=[0.01] * 8), dict(softcap=30.0), dict(softcap=30.0, slopes=[0.01] * 8)]
 
 
 @pytest.mark.parametrize("opts", SCORES, ids=lambda o: "-".join(o) or "plain")
@@ -72,3 +72,22 @@ def test_a_key_behind_a_row_changes_no_bit_of_it(dtype, hd, C, rows, opts):
     before = [r for r in range(s.M) if r != rows[0] - 1]
     assert torch.equal(out1[before], out[before]) and torch.equal(lse1[before], lse[before])
     assert not torch.equal(lse1[rows[0] - 1], lse[rows[0] - 1])
+
+
+@pytest.mark.parametrize("opts", SCORES, ids=lambda o: "-".join(o) or "plain")
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("C,rows", BLOCKS)
+def test_what_lies_in_unseen_places_changes_no_bit(dtype, C, rows, opts):
+    """Places of the pages that hold no key, and keys behind every row's window: NaN, zeros, infinities, large values."""
+    c = rising(74, dtype, 128, C, rows, window=90, **opts)
+    s, hidden = c.s, C[0] - 89
+    empty = torch.isnan(s.pool)
+    got = []
+    for val in (float("nan"), 0.0, float("inf"), -1e30):
+        s.pool[empty] = val
+        s.write(0, 0, np.full((hidden, 2, 128), val), np.full((hidden, 2, 128), val))
+        c.call()
+        got.append(bits(c))
+    for out, lse in got[1:]:
+        assert torch.equal(out, got[0][0]) and torch.equal(lse, got[0][1])
+    assert torch.isfinite(got[0][0]).all()
