@@ -852,7 +852,13 @@ __global__ void __launch_bounds__(256, 2) attend_tile_kernel(AttendArgs a, Atten
   for (int d = 0; d < HD / 32; ++d) o[d] = f32x16_t{};
   float mrun = -INFINITY, lrun = 0.f;  // the reference of the probabilities, their sum
   // plain scores stay unscaled (their factor is positive) until the exponent's multiply-add
-  const float c = MOD ? 1.f : a.scale * kLog2e, slack = 8.f / c;
+  const float c = MOD ? 1.f : a.scale * kLog2e;
+  float slack = 8.f / c;  // of the reference; -inf for a row whose scores are far from 0 (below)
+  // a score times its factor, rounded as it is, in no multiply-add
+  auto scaled = [&](float s) {
+#pragma clang fp contract(off)
+    return s * c;
+  };
   uint32_t infinite[2][HD / 64] = {};  // per element of o: whether it sums a value infinite upwards, downwards
 
   // this lane's source pieces of the direct loads: piece i of a page's block goes to LDS slot i, which
@@ -939,14 +945,29 @@ __global__ void __launch_bounds__(256, 2) attend_tile_kernel(AttendArgs a, Atten
     // what the others see.
     const bool within = mx <= mrun + slack;
     if (!__all(within)) {
-      const float mnew = within ? mrun : mx;
-      const float alpha = mnew == mrun ? 1.f : __builtin_amdgcn_exp2f((mrun - mnew) * c);
+      const float mnew = within ? mrun : fmaxf(mrun, mx);
+      const float alpha = mnew == mrun ? 1.f : __builtin_amdgcn_exp2f(scaled(mrun) - scaled(mnew));
       mrun = mnew;
       lrun *= alpha;
 #pragma unroll
       for (int d = 0; d < HD / 32; ++d) o[d] *= alpha;
+      // The exponent's multiply-add is off by the rounding of the reference: half a unit at 2^24, past all of fp32's
+      // exponents from 2^31 on.  A row that far comes here for each page: its scores are rounded like the reference and their
+      // differences handed on, in units of the scores, under a reference of 0.
+      if constexpr (!MOD) {
+        const float from = scaled(mrun), back = 1.f / c;
+        const bool far = fabsf(from) >= 0x1p24f && mrun != -INFINITY;
+        slack = far ? -INFINITY : 8.f / c;
+        if (__any(far)) {
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sc[kb][r] = far ? (scaled(sc[kb][r]) - from) * back : sc[kb][r];
+        }
+      }
     }
-    const float ref = mrun == -INFINITY ? 0.f : mrun * c;  // nothing seen yet: every probability is 2^-inf
+    // nothing seen yet: every probability is 2^-inf
+    const float ref = mrun == -INFINITY || slack == -INFINITY ? 0.f : scaled(mrun);
     float sum = 0.f;
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
@@ -1038,7 +1059,7 @@ __global__ void __launch_bounds__(256, 2) attend_tile_kernel(AttendArgs a, Atten
       o[d][r] += infinite_part(infinite[0][d / 2] >> (16 * (d % 2) + r), infinite[1][d / 2] >> (16 * (d % 2) + r));
 
   const float l = lrun + __shfl_xor(lrun, 32, kWave);
-  const float m = MOD ? mrun : mrun * (a.scale * kLog2e);
+  const float m = scaled(mrun);
   auto part_of = [&](int d, int r) { return f32x4_t{o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]}; };
   if (u.splits > 1) {
     if (!valid) return;
