@@ -293,8 +293,11 @@ int lsv_rope_init(lsv_rope* rope, int32_t layout, int32_t rot_dim, double base, 
  *   dtype           LSV_DTYPE_*;  n_heads up to 65535
  *   head_dim        a multiple of 8 up to LSV_ROPE_MAX_DIM, >= rot_dim
  *   d_positions     [rows] int32, nullable: the rows' positions (any int32); NULL: d_seq_len[b] + i
- *   d_row_offsets   [batch+1] int32, nullable with d_positions: then there are max_rows rows; a
- *                   last offset outside [0, max_rows] leaves every row as it was
+ *   d_row_offsets   [batch+1] int32, nullable with d_positions: then there are max_rows rows.  Rows
+ *                   before the first offset and from the last on stay as they were, and all of them
+ *                   unless 0 <= first <= last <= max_rows (with d_positions no other is read).
+ *                   Without d_positions so do the rows of a sequence that lsv_append_paged would
+ *                   refuse with LSV_ERR_INVALID_ARG, or whose positions pass 2^31 - 1
  *   d_seq_len       [batch] int32, read only without d_positions (else nullable)
  *   max_rows        host bound on the rows, 1..LSV_MAX_CHUNK_ROWS
  *   d_x, d_y        row arrays; d_y == d_x with equal strides rotates in place (other overlaps

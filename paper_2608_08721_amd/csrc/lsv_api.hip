@@ -395,7 +395,7 @@ int lsv_apply_rope(const lsv_rope* rope, int32_t dtype, int32_t n_heads, int32_t
   const int es = dtype == LSV_DTYPE_BF16 ? 2 : 4;
   if ((rc = check_rows("x", d_x, es, x_stride, width)) || (rc = check_rows("y", d_y, es, y_stride, width))) return rc;
   if (d_x == d_y && x_stride != y_stride) return fail(LSV_ERR_INVALID_ARG, "in place needs equal strides");
-  const lsv::RowArgs rows{d_seq_len, d_row_offsets, d_positions, batch, max_rows, max_rows, 0};
+  const lsv::RowArgs rows{d_seq_len, d_row_offsets, d_positions, batch, max_rows, max_rows, INT32_MAX};
   return hip_rc(lsv::launch_rope(rope_args(rope), dtype, n_heads, head_dim, rows, d_x, x_stride, d_y, y_stride,
                                  (hipStream_t)stream),
                 "apply_rope");

@@ -48,8 +48,8 @@ __host__ __device__ inline Units units_of(int layout, int rot, int hd, int n, bo
   return u;
 }
 
-// Rotate `nrow` rows of `heads` heads: from(r, h) and to(r, h) are head h of row r, pos(r) the row's
-// position.  Threads take (unit, row, head) with the unit fastest.  A thread owns both elements of its
+// Rotate `nrow` rows of `heads` heads: from(r, h) and to(r, h) are head h of row r, pos(r, p) sets the row's
+// position, false: the row stays as it is.  Threads take (unit, row, head) with the unit fastest.  A thread owns both elements of its
 // pairs, so that rotating in place is safe; the unrotated tail goes over only where `copy` says so.
 template <typename T, bool VEC, bool HALF, typename From, typename To, typename Pos>
 LSV_DEV void rotate_rows(const RopeArgs& rope, int nrow, int heads, int hd, bool copy, From from, To to, Pos pos) {
@@ -69,7 +69,8 @@ LSV_DEV void rotate_rows(const RopeArgs& rope, int nrow, int heads, int hd, bool
 #pragma unroll
   for (int k = 0; k < PAIRS; ++k) f[k] = turns ? rope.half_turns[(HALF || !VEC ? u * N : u * N / 2) + k] : 0.0;
   for (int r = r0; r < nrow; r += rows) {
-    const int p = pos(r);
+    int p;
+    if (!pos(r, p)) continue;
     float2 c[PAIRS];
     bool formed = false;
     for (int h = h0; h < heads; h += lanes * BATCH) {
@@ -125,24 +126,33 @@ static bool aligned16(const void* p, int64_t stride, size_t es) {
 template <typename T, bool VEC, bool HALF>
 __global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs rope, RowArgs rows, int group, int lot, const T* x,
                                                         int64_t xs, T* y, int64_t ys, int heads, int hd, bool copy) {
-  __shared__ int end[LSV_MAX_BATCH], base[LSV_MAX_BATCH];  // the row behind a sequence; its position minus its row
+  // per sequence: its first row; the row behind it and those before it; its position minus its row
+  __shared__ int begin[LSV_MAX_BATCH], end[LSV_MAX_BATCH], base[LSV_MAX_BATCH];
+  const int first = rows.row_offsets ? GL(rows.row_offsets)[0] : 0;
   const int M = rows.row_offsets ? GL(rows.row_offsets)[rows.batch] : rows.max_rows;
-  const int m0 = blockIdx.x * group, h0 = blockIdx.y * lot;
-  if (M > rows.max_rows || m0 >= M) return;
-  if (!rows.positions) {
-    const int t = threadIdx.x;
+  if (!rows.positions) {  // its loads go out with those of first and M
+    const SeqRows s = seq_rows(rows);
+    const int behind = wave_scan_max(s.rows > 0 ? s.r0 + s.rows : 0), t = threadIdx.x;
     if (t < rows.batch) {
-      end[t] = GL(rows.row_offsets)[t + 1];
-      base[t] = GL(rows.seq_len)[t] - GL(rows.row_offsets)[t];
+      begin[t] = s.r0;
+      end[t] = behind;
+      base[t] = s.C - s.r0;
     }
     __syncthreads();
   }
-  auto pos = [&](int r) {
+  if (first < 0 || first > M || M > rows.max_rows) return;
+  const int m0 = first + blockIdx.x * group, h0 = blockIdx.y * lot;
+  if (m0 >= M) return;
+  auto pos = [&](int r, int& p) {
     const int m = m0 + r;
-    if (rows.positions) return GL(rows.positions)[m];
-    int b = 0;
-    while (b + 1 < rows.batch && end[b] <= m) ++b;
-    return base[b] + m;
+    if (rows.positions) {
+      p = GL(rows.positions)[m];
+      return true;
+    }
+    int b = 0;  // the ends rise: as many sequences lie before the row as end at or before it
+    for (int k = 0; k + 1 < rows.batch; ++k) b += end[k] <= m ? 1 : 0;
+    p = base[b] + m;
+    return m >= begin[b] && m < end[b];  // else a refused sequence's row
   };
   const T* px = x + m0 * xs + (int64_t)h0 * hd;
   T* py = y + m0 * ys + (int64_t)h0 * hd;
@@ -240,7 +250,10 @@ __global__ void __launch_bounds__(kThreads) append_kernel(RopeArgs rope, AppendA
   rotate_rows<T, VEC, HALF>(rope, n, group + (there ? 1 : 0), HD, true,
                             [&](int r, int h) { return h < group ? q + r * a.qs + (int64_t)h * HD : k + r * a.ks; },
                             [&](int r, int h) { return h < group ? q_out + r * a.qos + (int64_t)h * HD : k_out + r * HD; },
-                            [&](int r) { return a.rows.positions ? GL(a.rows.positions)[m0 + r] : first + r; });
+                            [&](int r, int& p) {
+                              p = a.rows.positions ? GL(a.rows.positions)[m0 + r] : first + r;
+                              return true;
+                            });
   if (!there) return;
   if constexpr (VEC) {
 #pragma unroll

@@ -256,3 +256,46 @@ def test_rope_and_append_on_another_stream():
     assert s.status.tolist() == [0, 0] and torch.equal(q, y[:, :256])
     k = np.concatenate([s.read(b, c + n)[0][c:] for b, (c, n) in enumerate(((60, 9), (3, 1)))])
     assert np.array_equal(k.reshape(10, 128), f64(y[:, 256:384]))
+
+
+@pytest.mark.parametrize("positions", [False, True])
+@pytest.mark.parametrize("dtype,rot,M", [("bf16", 64, 40), ("f32", 64, 40), ("bf16", 12, 700), ("f32", 64, 3000)])
+def test_rope_takes_the_rows_that_the_offsets_name(dtype, rot, M, positions):
+    """Offsets that begin behind 0: the rows before the first are as they were, in place too."""
+    t, code, half = DT[dtype]
+    rng = np.random.default_rng(5)
+    x = torch.tensor(rng.normal(size=(M + 5, 128)), device="cuda").to(t)
+    r, first = make_rope(rot), M // 3
+    C, off = [11, 500, 7], [first, first + 4, first + 4, M]
+    seq = i32(C)
+    whole = np.concatenate([np.full(first, 3), 11 + np.arange(4), 7 + np.arange(M - first - 4)])
+    want = x.clone()
+    lsv.lsv_apply_rope(r, code, 2, 64, 1, None, None, i32(whole), M, x, 128, want, 128)
+    want[:first] = x[:first]
+    y = x.clone()
+    args = (None, i32(off), i32(whole)) if positions else (seq, i32(off), None)
+    lsv.lsv_apply_rope(r, code, 2, 64, 3, *args, M + 5, y, 128, y, 128)
+    torch.cuda.synchronize()
+    assert torch.equal(y, want)
+
+
+def test_rope_leaves_refused_sequences_alone():
+    """Offsets and lengths that the append refuses: those rows stay as they were, the others turn."""
+    r = make_rope()
+    x = torch.tensor(np.random.default_rng(6).normal(size=(12, 64)), device="cuda").float()
+
+    def turned(pos):
+        y = x.clone()
+        lsv.lsv_apply_rope(r, lsv.LSV_DTYPE_F32, 1, 64, 1, None, None, i32(pos), 12, x, 64, y, 64)
+        return y
+    for C, off, rows in (([5, -1, 9], [0, 2, 7, 12], {0: (0, 2), 2: (7, 12)}),     # a negative length
+                         ([5, 6, 9], [0, 9, 3, 12], {0: (0, 9)}),                  # decreasing, then behind an earlier offset
+                         ([5, 2 ** 31 - 3, 9], [0, 2, 7, 12], {0: (0, 2), 2: (7, 12)}),  # positions past 32 bits
+                         ([5, 6, 9], [-1, 2, 7, 12], {}), ([5, 6, 9], [13, 2, 7, 12], {}), ([5, 6, 9], [0, 2, 7, 13], {})):
+        want = x.clone()
+        for b, (a, z) in rows.items():
+            want[a:z] = turned(C[b] + np.arange(12) - a)[a:z]
+        y = x.clone()
+        lsv.lsv_apply_rope(r, lsv.LSV_DTYPE_F32, 1, 64, 3, i32(C), i32(off), None, 12, y, 64, y, 64)
+        torch.cuda.synchronize()
+        assert torch.equal(y, want), (C, off)
