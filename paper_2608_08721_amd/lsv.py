@@ -60,16 +60,26 @@ class Rope(ctypes.Structure):
 
 
 class AttendOptions(ctypes.Structure):
-    """lsv_attend_options: zero for a default; the d_ fields take addresses (tensor.data_ptr(), the
-    tensors kept alive by the caller)."""
+    """lsv_attend_options: zero for a default.  The d_ fields take tensors, which lsv_attend_paged checks and
+    the options keep alive, or addresses, which go through unchecked (the caller keeps the memory)."""
     _fields_ = [
         ("scale", ctypes.c_float), ("softcap", ctypes.c_float), ("window", ctypes.c_int32),
         ("reserved0", ctypes.c_int32), ("d_slopes", ctypes.c_void_p), ("d_key_start", ctypes.c_void_p),
         ("d_prefix_len", ctypes.c_void_p),
     ]
 
+    def __setattr__(self, name, value):
+        if name.startswith("d_"):
+            self.__dict__.pop(name, None)
+            if value is not None and not isinstance(value, int):
+                self.__dict__[name] = value  # behind the field of that name, which holds the address
+                value = value.data_ptr()
+        super().__setattr__(name, value)
+
 
 _lib = None
+_C = _I32 = _F32 = None  # torch._C and torch's types, from load() on: an import statement takes 0.3 us of a 6 us call
+_TYPES = {}              # torch's type of an LSV_DTYPE_*
 
 
 def load(path=LIB_PATH):
@@ -79,8 +89,11 @@ def load(path=LIB_PATH):
         return _lib
     if not os.path.exists(path):
         raise ImportError(f"{path} is not built: run __graft_entry__.build() (hipcc, gfx950)")
+    global _C, _I32, _F32
     try:  # torch first, so the process holds exactly one HIP runtime (torch's), matched by soname
-        import torch  # noqa: F401
+        import torch
+        _C, _I32, _F32 = torch._C, torch.int32, torch.float32
+        _TYPES.update({LSV_DTYPE_F32: torch.float32, LSV_DTYPE_BF16: torch.bfloat16})
     except ImportError:
         pass
     lib = ctypes.CDLL(path)
@@ -158,27 +171,46 @@ def _need(t, name, n, dtype):
                                             f"{t.dtype} {tuple(t.shape)} on {t.device}")
 
 
-_C = None  # torch._C, once a tensor has come by: an import statement takes 0.3 us of a 6 us call
+ROWS = -1  # the length of row arrays, some stride apart, which is the device's to know
 
 
 def _here(stream, *args):
-    """The stream's handle (None: the current stream) and the addresses of tensor arguments, which must lie
-    on the current device, where the call runs; raw integer addresses are passed through unchecked."""
-    global _C
+    """The stream's handle (None: the current stream) and the addresses of tensor arguments, each given as (name, tensor,
+    type, least number of elements).  They must lie on the current device, where the call runs, have that type (None: any)
+    and, but for ROWS, be contiguous: a length of another type would be read as another length.  Raw integer addresses
+    are passed through unchecked."""
     dev, out = None, [None]
-    for x in args:
+    for name, x, dtype, n in args:
         if x is not None and not isinstance(x, int):
             on = x.get_device()
             if dev is None and on >= 0:
-                if _C is None:
-                    from torch import _C
                 dev = _C._cuda_getDevice()  # torch.cuda.current_device() without its look for a first use
             if on != dev:
-                raise LsvError(LSV_ERR_INVALID_ARG, f"a tensor on {x.device}, not on the current GPU")
+                raise LsvError(LSV_ERR_INVALID_ARG, f"{name}: a tensor on {x.device}, not on the current GPU")
+            if dtype is not None and x.dtype is not dtype or n >= 0 and (x.numel() < n or not x.is_contiguous()):
+                _refuse(name, x, dtype, n, "elements")
             x = x.data_ptr()
         out.append(x)
     out[0] = _C._cuda_getCurrentRawStream(dev) if stream is None and dev is not None else _stream(stream)
     return out
+
+
+def _refuse(name, x, dtype, n, of):
+    raise LsvError(LSV_ERR_INVALID_ARG, f"{name}: need a {dtype or 'contiguous'} tensor"
+                                        f"{f', contiguous, of >= {n} {of}' if n >= 0 else ''}, got {x.dtype} {tuple(x.shape)}")
+
+
+def _holds(name, x, nbytes, dtype):
+    """A buffer that a call takes whole holds nbytes, of that type or of single bytes (None: any type)."""
+    if x is not None and not isinstance(x, int) and (
+            x.nbytes < nbytes or not x.is_contiguous() or
+            dtype is not None and x.dtype is not dtype and x.element_size() != 1):
+        _refuse(name, x, dtype, nbytes, "bytes")
+
+
+def _pool_bytes(cfg, n_pages):
+    return (2 * LSV_KV_PAGE * (2 if cfg.dtype == LSV_DTYPE_BF16 else 4) * cfg.n_layers * n_pages * cfg.n_kv_heads *
+            cfg.head_dim)
 
 
 def _check(rc):
@@ -327,20 +359,27 @@ def lsv_rope_init(rope, layout, rot_dim, base, scaling=LSV_ROPE_PLAIN, factor=1.
 
 def lsv_apply_rope(rope, dtype, n_heads, head_dim, batch, seq_len, row_offsets, positions, max_rows, x, x_stride, y,
                    y_stride, stream=None):
-    stream, seq_len, row_offsets, positions, x, y = _here(stream, seq_len, row_offsets, positions, x, y)
-    _check(load().lsv_apply_rope(ctypes.byref(rope), dtype, n_heads, head_dim, batch, seq_len, row_offsets, positions,
-                                 max_rows, x, x_stride, y, y_stride, stream))
+    lib, t = load(), _TYPES.get(dtype)
+    stream, seq_len, row_offsets, positions, x, y = _here(
+        stream, ("seq_len", seq_len, _I32, batch if positions is None else 0), ("row_offsets", row_offsets, _I32, batch + 1),
+        ("positions", positions, _I32, max_rows if row_offsets is None else 0), ("x", x, t, ROWS), ("y", y, t, ROWS))
+    _check(lib.lsv_apply_rope(ctypes.byref(rope), dtype, n_heads, head_dim, batch, seq_len, row_offsets, positions,
+                              max_rows, x, x_stride, y, y_stride, stream))
 
 
 def lsv_append_paged(cfg, layer, kv_pool, n_pages, page_table, max_pages, batch, seq_len, row_offsets, positions,
                      max_rows, max_ctx, rope, q, q_stride, q_out, q_out_stride, k, k_stride, v, v_stride, status,
                      stream=None):
+    lib, t, pool = load(), _TYPES.get(cfg.dtype), kv_pool
     stream, kv_pool, page_table, seq_len, row_offsets, positions, q, q_out, k, v, status = _here(
-        stream, kv_pool, page_table, seq_len, row_offsets, positions, q, q_out, k, v, status)
-    _check(load().lsv_append_paged(ctypes.byref(cfg), layer, kv_pool, n_pages, page_table, max_pages, batch, seq_len,
-                                   row_offsets, positions, max_rows, max_ctx,
-                                   ctypes.byref(rope) if rope is not None else None, q, q_stride, q_out, q_out_stride, k,
-                                   k_stride, v, v_stride, status, stream))
+        stream, ("kv_pool", kv_pool, None, ROWS), ("page_table", page_table, _I32, batch * max_pages),
+        ("seq_len", seq_len, _I32, batch), ("row_offsets", row_offsets, _I32, batch + 1), ("positions", positions, _I32, 0),
+        ("q", q, t, ROWS), ("q_out", q_out, t, ROWS), ("k", k, t, ROWS), ("v", v, t, ROWS), ("status", status, _I32, batch))
+    _holds("kv_pool", pool, _pool_bytes(cfg, n_pages), t)
+    _check(lib.lsv_append_paged(ctypes.byref(cfg), layer, kv_pool, n_pages, page_table, max_pages, batch, seq_len,
+                                row_offsets, positions, max_rows, max_ctx,
+                                ctypes.byref(rope) if rope is not None else None, q, q_stride, q_out, q_out_stride, k,
+                                k_stride, v, v_stride, status, stream))
 
 
 def lsv_attend_workspace_bytes(cfg, batch, max_rows, max_rows_per_seq, max_ctx):
@@ -350,12 +389,20 @@ def lsv_attend_workspace_bytes(cfg, batch, max_rows, max_rows_per_seq, max_ctx):
 def lsv_attend_paged(cfg, layer, kv_pool, n_pages, page_table, max_pages, batch, seq_len, row_offsets, max_rows,
                      max_rows_per_seq, max_ctx, options, q, q_stride, out, out_stride, lse, status, ws, ws_bytes,
                      stream=None):
-    stream, kv_pool, page_table, seq_len, row_offsets, q, out, lse, status, ws = _here(
-        stream, kv_pool, page_table, seq_len, row_offsets, q, out, lse, status, ws)
-    _check(load().lsv_attend_paged(ctypes.byref(cfg), layer, kv_pool, n_pages, page_table, max_pages, batch, seq_len,
-                                   row_offsets, max_rows, max_rows_per_seq, max_ctx,
-                                   ctypes.byref(options) if options is not None else None, q, q_stride, out, out_stride,
-                                   lse, status, ws, ws_bytes, stream))
+    lib, t, pool, space = load(), _TYPES.get(cfg.dtype), kv_pool, ws
+    kept = options.__dict__ if options is not None else {}
+    stream, kv_pool, page_table, seq_len, row_offsets, q, out, lse, status, ws, *_ = _here(
+        stream, ("kv_pool", kv_pool, None, ROWS), ("page_table", page_table, _I32, batch * max_pages),
+        ("seq_len", seq_len, _I32, batch), ("row_offsets", row_offsets, _I32, batch + 1), ("q", q, t, ROWS),
+        ("out", out, t, ROWS), ("lse", lse, _F32, 0), ("status", status, _I32, batch), ("ws", ws, None, ROWS),
+        ("d_slopes", kept.get("d_slopes"), _F32, cfg.n_q_heads), ("d_key_start", kept.get("d_key_start"), _I32, 0),
+        ("d_prefix_len", kept.get("d_prefix_len"), _I32, batch))
+    _holds("kv_pool", pool, _pool_bytes(cfg, n_pages), t)
+    _holds("ws", space, ws_bytes, None)
+    _check(lib.lsv_attend_paged(ctypes.byref(cfg), layer, kv_pool, n_pages, page_table, max_pages, batch, seq_len,
+                                row_offsets, max_rows, max_rows_per_seq, max_ctx,
+                                ctypes.byref(options) if options is not None else None, q, q_stride, out, out_stride,
+                                lse, status, ws, ws_bytes, stream))
 
 
 def lsv_set_timing_events(kernel, events, n_slots, record_flags=0):

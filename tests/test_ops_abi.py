@@ -183,3 +183,73 @@ def test_tensors_elsewhere_are_refused(lib):  # noqa: F811
 def test_struct_sizes():
     assert ctypes.sizeof(lsv.Rope) == 16 + 8 * lsv.LSV_ROPE_MAX_DIM // 2
     assert ctypes.sizeof(lsv.AttendOptions) == 40
+
+
+def test_tensors_of_another_type_or_length_are_refused(lib, monkeypatch):  # noqa: F811
+    """The binding's own checks, on tensors that say they lie on the current GPU: none of these calls reaches the library,
+    whose refusals (a layer out of range, no rows) show that the right tensors pass."""
+    torch = pytest.importorskip("torch")
+
+    class Here(torch.Tensor):
+        def get_device(self):
+            return 0
+
+    class Driver:
+        _cuda_getDevice = staticmethod(lambda: 0)
+    monkeypatch.setattr(lsv, "_C", Driver)
+    on = lambda *shape, t=torch.int32: torch.zeros(shape, dtype=t).as_subclass(Here)  # noqa: E731
+    f32, bf16, u8 = torch.float32, torch.bfloat16, torch.uint8
+    cfg, B, P, n_pages = tiny_cfg(), 2, 4, 3  # fp32, 4 heads of 64, two layers
+    pool = on(2 * 2 * n_pages * 4 * 64 * 64, t=f32)
+    wrong = dict(seq=[on(B, t=torch.int64), on(B - 1), on(2 * B)[::2]], off=[on(B + 1, t=torch.int64), on(B)],
+                 table=[on(B, P, t=torch.int64), on(B, P - 1), on(B, P + 1)[:, :P]], status=[on(B, t=f32), on(1)],
+                 pool=[on(2, 2, n_pages, 4, 4096, t=bf16), on(2, 2, n_pages - 1, 4, 4096, t=f32),
+                       on(pool.nbytes - 1, t=u8), on(2, 2, n_pages, 4, 4096, t=torch.int32)],
+                 rows=[on(8, 256, t=bf16), on(8, 256, t=torch.float64)], pos=[on(8, t=torch.int64), on(16)[::2]],
+                 lse=[on(8, 4, t=bf16)], ws=[on(64, t=u8)], d_slopes=[on(4, t=torch.float64), on(3, t=f32)],
+                 d_key_start=[on(8, t=torch.int64)], d_prefix_len=[on(B, t=torch.int64), on(1)])
+    right = dict(seq=on(B), off=on(B + 1), table=on(B, P), status=on(B), pool=pool, rows=on(8, 256, t=f32), pos=on(8),
+                 lse=on(8, 4, t=f32), ws=on(1 << 20, t=u8), d_slopes=on(4, t=f32), d_key_start=on(8), d_prefix_len=on(B))
+
+    def rotate(a, dtype=lsv.LSV_DTYPE_F32):
+        lsv.lsv_apply_rope(rope(), dtype, 4, 64, B, a["seq"], a["off"], a["pos"], 0, a["rows"], 256, a["rows"],
+                           256, S)
+
+    def append(a):
+        lsv.lsv_append_paged(cfg, 9, a["pool"], n_pages, a["table"], P, B, a["seq"], a["off"], a["pos"], 8, 256, rope(),
+                             a["rows"], 256, a["rows"], 256, a["rows"], 256, a["rows"], 256, a["status"], S)
+
+    def attend(a):
+        o = lsv.AttendOptions(d_slopes=a["d_slopes"])
+        o.d_key_start, o.d_prefix_len = a["d_key_start"], a["d_prefix_len"]
+        lsv.lsv_attend_paged(cfg, 9, a["pool"], n_pages, a["table"], P, B, a["seq"], a["off"], 8, 4, 256, o, a["rows"], 256,
+                             a["rows"], 256, a["lse"], a["status"], a["ws"], 1 << 20, S)
+
+    for call, names, last in ((rotate, "off pos rows", "max_rows"), (append, "pool table seq off pos rows status", "layer 9"),
+                              (attend, "pool table seq off rows lse status ws d_slopes d_key_start d_prefix_len", "layer 9")):
+        assert last in expect(BAD, call, right)
+        assert last in expect(BAD, call, dict(right, pool=on(pool.nbytes, t=u8)))
+        for name in names.split():
+            for x in wrong[name]:
+                assert "need a" in expect(BAD, call, dict(right, **{name: x})), (call, name, x.dtype, x.shape)
+    # lengths in place of positions, and rows of the other type
+    assert "need a" in expect(BAD, rotate, dict(right, pos=None, seq=on(B, t=torch.int64)))
+    assert "need a" in expect(BAD, rotate, right, lsv.LSV_DTYPE_BF16)
+
+
+def test_options_keep_their_tensors():
+    torch = pytest.importorskip("torch")
+    import gc
+    import weakref
+    o = lsv.AttendOptions(softcap=2.0)
+    x = torch.zeros(4)
+    o.d_slopes, seen = x, weakref.ref(x)
+    at = x.data_ptr()
+    del x
+    gc.collect()
+    assert seen() is not None and o.d_slopes == at and o.softcap == 2.0
+    o.d_slopes = at  # an address from now on
+    gc.collect()
+    assert seen() is None and o.d_slopes == at
+    o.d_slopes = None
+    assert o.d_slopes is None
