@@ -274,7 +274,8 @@ int lsv_verify_paged(const lsv_model_config* cfg, const void* d_packed, void* d_
  * factor is read from LINEAR on, low, high and original_ctx by BANDS and RAMP.
  * LSV_ERR_INVALID_ARG: rope NULL; unknown layout or scaling; rot_dim odd or outside
  * [2, LSV_ROPE_MAX_DIM]; base, factor or amplitude not finite and positive (RAMP: base > 1; NTK:
- * rot_dim > 2); original_ctx < 1 or not 0 < low < high where they are read. */
+ * rot_dim > 2); original_ctx < 1 or not 0 < low < high where they are read; frequencies, or angles
+ * up to position 2^31, that binary64 does not hold. */
 enum { LSV_ROPE_HALF = 0, LSV_ROPE_INTERLEAVED = 1 };
 enum { LSV_ROPE_PLAIN = 0, LSV_ROPE_LINEAR = 1, LSV_ROPE_NTK = 2, LSV_ROPE_BANDS = 3, LSV_ROPE_RAMP = 4 };
 enum { LSV_ROPE_MAX_DIM = 256 };

@@ -292,7 +292,8 @@ int check_rope(const lsv_rope* r, int head_dim) {
     return fail(LSV_ERR_INVALID_ARG, "bad rope: layout %d, rot_dim %d (even, 2..%d, <= head_dim %d), amplitude %g",
                 r->layout, r->rot_dim, (int)LSV_ROPE_MAX_DIM, head_dim, (double)r->amplitude);
   for (int j = 0; j < r->rot_dim / 2; ++j)
-    if (!isfinite(r->freq[j])) return fail(LSV_ERR_INVALID_ARG, "rope: freq[%d] is not finite", j);
+    if (!isfinite(r->freq[j] * 0x1p31))  // the angle of the last position
+      return fail(LSV_ERR_INVALID_ARG, "rope: freq[%d] is not finite, or its angles are not", j);
   return LSV_OK;
 }
 
@@ -350,10 +351,7 @@ int lsv_rope_init(lsv_rope* rope, int32_t layout, int32_t rot_dim, double base, 
   const bool blend = scaling == LSV_ROPE_BANDS || scaling == LSV_ROPE_RAMP;
   if (blend && (original_ctx < 1 || !(low > 0.0) || !(high > low) || !isfinite(high)))
     return fail(LSV_ERR_INVALID_ARG, "need original_ctx >= 1 and 0 < low < high");
-  rope->layout = layout;
-  rope->rot_dim = rot_dim;
-  rope->amplitude = (float)amplitude;
-  rope->reserved0 = 0.f;
+  lsv_rope r = {layout, rot_dim, (float)amplitude, 0.f, {}};
   if (scaling == LSV_ROPE_NTK) base *= pow(factor, (double)rot_dim / (rot_dim - 2));
   auto index_of = [&](double turns) { return rot_dim * log(original_ctx / (2.0 * M_PI * turns)) / (2.0 * log(base)); };
   double first = 0.0, width = 1.0;
@@ -370,8 +368,12 @@ int lsv_rope_init(lsv_rope* rope, int32_t layout, int32_t rot_dim, double base, 
       const double keep = fmin(fmax(at, 0.0), 1.0);
       f = keep * f + (1.0 - keep) * f / factor;
     }
-    rope->freq[j] = f;
+    r.freq[j] = f;
   }
+  if (!isfinite(base)) return fail(LSV_ERR_INVALID_ARG, "the stretched base is not finite");
+  const int rc = check_rope(&r, LSV_ROPE_MAX_DIM);
+  if (rc) return rc;
+  *rope = r;
   return ok();
 }
 

@@ -253,3 +253,17 @@ def test_options_keep_their_tensors():
     assert seen() is None and o.d_slopes == at
     o.d_slopes = None
     assert o.d_slopes is None
+
+
+def test_frequencies_that_binary64_does_not_hold(lib):  # noqa: F811
+    """lsv_rope_init refuses what lsv_apply_rope could not use or would turn into other frequencies, and leaves the
+    handle as it was; so does a call with such a handle written by hand."""
+    r = lsv.Rope()
+    for args in ((0, 64, 1e300, lsv.LSV_ROPE_NTK, 1e9), (0, 64, 1e4, lsv.LSV_ROPE_LINEAR, 1e-309),
+                 (0, 64, 1e4, lsv.LSV_ROPE_BANDS, 1e-309, 1.0, 4.0, 8192), (0, 256, 1e-308)):  # (1e-308)^(-254/256) = 4e305
+        expect(BAD, lsv.lsv_rope_init, r, *args)
+        assert bytes(r) == bytes(ctypes.sizeof(r))
+    lsv.lsv_rope_init(r, 0, 64, 1e-290)
+    ok = [rope(), 1, 4, 64, 2, 16, 16, None, 8, 16, 256, 32, 256, S]
+    ok[0].freq[3] = -1e300
+    assert "freq[3]" in expect(BAD, lsv.lsv_apply_rope, *ok)
