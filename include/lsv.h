@@ -360,7 +360,7 @@ int lsv_append_paged(const lsv_model_config* cfg, int32_t layer, void* d_kv_pool
  *                     entry point alone; it carries nothing from one call to the next and serves
  *                     calls of any smaller size
  * lsv_attend_workspace_bytes returns 0 for bounds that lsv_attend_paged refuses: those above, and
- * (LSV_ERR_UNSUPPORTED) calls of 2^30 query vectors of a kv head, or whose tiles of 16 to 128 of them
+ * (LSV_ERR_UNSUPPORTED) more than 65535 kv heads, calls of 2^30 query vectors of a kv head, or whose tiles of 16 to 128 of them
  * would walk 2^30 pages of max_ctx in all, which is far past what a call should hold. */
 typedef struct lsv_attend_options {
   float scale;

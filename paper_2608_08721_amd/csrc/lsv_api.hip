@@ -442,7 +442,7 @@ size_t lsv_attend_workspace_bytes(const lsv_model_config* cfg, int32_t batch, in
                                   int32_t max_rows_per_seq, int32_t max_ctx) {
   if (check_config(cfg) != LSV_OK || batch < 1 || batch > LSV_MAX_BATCH || max_rows < 1 ||
       max_rows > LSV_MAX_CHUNK_ROWS || max_rows_per_seq < 1 || max_rows_per_seq > max_rows || max_ctx < 1 ||
-      max_ctx > (1 << 20) * LSV_KV_PAGE)
+      max_ctx > (1 << 20) * LSV_KV_PAGE || cfg->n_kv_heads > 65535)
     return 0;
   if (!lsv::attend_fits(lsv::shape_of(cfg), batch, max_rows, max_rows_per_seq, max_ctx)) return 0;
   return lsv::attend_workspace_bytes(lsv::shape_of(cfg), batch, max_rows, max_rows_per_seq, max_ctx);

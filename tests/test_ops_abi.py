@@ -267,3 +267,9 @@ def test_frequencies_that_binary64_does_not_hold(lib):  # noqa: F811
     ok = [rope(), 1, 4, 64, 2, 16, 16, None, 8, 16, 256, 32, 256, S]
     ok[0].freq[3] = -1e300
     assert "freq[3]" in expect(BAD, lsv.lsv_apply_rope, *ok)
+
+
+def test_no_workspace_for_head_counts_that_are_refused(lib):  # noqa: F811
+    cfg = lambda n: tiny_cfg(n_q_heads=n, n_kv_heads=n, head_dim=64, d_model=64)  # noqa: E731
+    assert lsv.lsv_attend_workspace_bytes(cfg(65536), 2, 8, 4, 256) == 0
+    assert lsv.lsv_attend_workspace_bytes(cfg(65535), 2, 8, 4, 256) > 0
