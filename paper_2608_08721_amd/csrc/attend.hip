@@ -1166,7 +1166,8 @@ HostPlan host_plan(int dtype, int hd, int nq, int nkv, int batch, int max_rows, 
   p.tiles = dtype == LSV_DTYPE_BF16 && per_seq > 32;
   // fp32 is bound by its matrix instructions: two tiles a wave pay from long chunks on, at head dimension 128
   // (300 rows behind 3000, group 4: 65 us against 70; 8 rows: 24 against 20; head dimension 64: 41 against 29)
-  p.tile = p.tiles ? kTileQ : per_seq > (dtype == LSV_DTYPE_BF16 ? 16 : hd == 128 ? kLongF32 : per_seq) ? 32 : 16;
+  const bool two = dtype == LSV_DTYPE_BF16 ? per_seq > 16 : hd == 128 && per_seq > kLongF32;
+  p.tile = p.tiles ? kTileQ : two ? 32 : 16;
   p.target = p.tiles || hd == 128 ? 512 : 1024;  // the workgroups that the chip holds at once
   p.least = dtype == LSV_DTYPE_BF16 ? kStreamWaves : 1;  // a step for each wave
   // tiles of sequences that share max_rows rows, each sequence's last one begun
@@ -1209,12 +1210,13 @@ size_t attend_workspace_bytes(const Shape& s, int batch, int max_rows, int max_r
 template <typename T, int HD, int MOD>
 static void launch_main(const AttendArgs& a, const HostPlan& p, const AttendPlan& pl, hipStream_t st) {
   const dim3 units((unsigned)p.units);
-  if (!p.tiles) {
-    if (p.tile == 32) hipLaunchKernelGGL((attend_stream_kernel<T, HD, 2, MOD>), units, dim3(64 * kStreamWaves), 0, st, a, pl);
-    else hipLaunchKernelGGL((attend_stream_kernel<T, HD, 1, MOD>), units, dim3(64 * kStreamWaves), 0, st, a, pl);
-  } else if constexpr (sizeof(T) == 2) {
-    hipLaunchKernelGGL((attend_tile_kernel<HD, MOD>), units, dim3(256), 0, st, a, pl);
+  if constexpr (sizeof(T) == 2) {
+    if (p.tiles) hipLaunchKernelGGL((attend_tile_kernel<HD, MOD>), units, dim3(256), 0, st, a, pl);
   }
+  if constexpr (sizeof(T) == 2 || HD == 128) {  // as in host_plan
+    if (p.tile == 32) hipLaunchKernelGGL((attend_stream_kernel<T, HD, 2, MOD>), units, dim3(64 * kStreamWaves), 0, st, a, pl);
+  }
+  if (p.tile == 16) hipLaunchKernelGGL((attend_stream_kernel<T, HD, 1, MOD>), units, dim3(64 * kStreamWaves), 0, st, a, pl);
 }
 
 template <typename T, int HD>
