@@ -131,3 +131,58 @@ def test_rows_beside_refused_sequences():
                 else:
                     x = f64(c.out[mine, :c.W]).reshape(-1, 8, 128)
                     assert np.all(np.abs(x - want["out"][mine]) <= bound[mine])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("nq,nkv,hd,C,rows,opts", [
+    (128, 1, 128, [700, 3], [1, 1], {}), (71, 1, 64, [300, 0, 63], [1, 2, 1], dict(softcap=20.0)),
+    (300, 2, 64, [130], [3], dict(window=40)), (33, 1, 128, [5000], [1], {}), (200, 1, 64, [0], [1], {})])
+def test_groups_of_more_heads_than_a_tile_holds_rows(dtype, nq, nkv, hd, C, rows, opts):
+    """One row's query heads fill tiles, or pass them."""
+    c = Case(87, nq, nkv, hd, dtype, C, rows, **opts)
+    c.call()
+    c.check()
+
+
+@pytest.mark.parametrize("dtype,nq,nkv", [("bf16", 8, 2), ("f32", 4, 4)])
+def test_sixty_four_ragged_sequences(dtype, nq, nkv):
+    """The most sequences of a call: empty ones among single tokens and chunks, at the ends too."""
+    rows = [0, 1, 40, 3, 0, 70, 2, 1] * 8
+    c = Case(88, nq, nkv, 64, dtype, [(37 * b) % 500 for b in range(64)], rows)
+    c.call()
+    c.check()
+
+
+def test_one_graph_under_changing_lengths():
+    """A call captured once, replayed under lengths for which the device chooses other cuts: whole tiles, a last round in
+    parts, splits by length, no rows; eager work between."""
+    c = Case(89, 96, 32, 64, "bf16", [600, 700], [725, 300])
+    M, per, ctx = c.bounds
+    bounds = (M, 725, ctx)
+    C, off, seen = i32([0, 0]), i32([0, 0, 0]), set()
+    cases = [([600, 700], [725, 300]), ([1300, 60], [25, 30]), ([600, 0], [725, 0]), ([0, 0], [100, 0]), ([5, 5], [0, 0]),
+             ([600, 700], [725, 20])]
+    c.dev = C, off
+    graph = None
+    for lens, rows in cases + cases[::-1]:
+        C.copy_(i32(lens))
+        off.copy_(i32(runtime.row_offsets_of(rows)))
+        c.out.fill_(7.0)
+        c.lse.fill_(7.0)
+        c.call(bounds=bounds)
+        seen.add(tuple(cut_of(c)))
+        want, lse = c.out.clone(), c.lse.clone()
+        if graph is None:
+            torch.cuda.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                c.call(bounds=bounds)
+        for _ in range(3):
+            c.out.fill_(7.0)
+            c.lse.fill_(7.0)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert c.s.status.tolist() == [0, 0]
+            assert torch.equal(c.out, want) and torch.equal(c.lse, lse)
+        assert (want[sum(rows):] == 7.0).all() and (want[:sum(rows), :c.W] != 7.0).any() == (sum(rows) > 0)
+    assert len({(pps != ALL, parts > 1) for pps, _, parts in seen}) == 3, seen
