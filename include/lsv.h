@@ -150,8 +150,8 @@ size_t lsv_kv_cache_bytes(const lsv_model_config* cfg, int32_t batch, int32_t ca
  * i.e. a page is laid out like a block of the slab cache above.  Position pos of sequence b lives in page
  * d_page_table[b * max_pages + pos / 64] at j = pos % 64; a table entry outside
  * [0, n_pages) reads as zeros and is never written.  The caller owns the pool and the table
- * (any page order; pages need not be contiguous).  A layer's K pool must stay under 2 GiB
- * ((n_pages + 1) * n_kv_heads * 64 * head_dim * element size < 2^31).
+ * (any page order; pages need not be contiguous).  For lsv_verify_paged and lsv_commit_tree_paged a
+ * layer's K pool must stay under 2 GiB ((n_pages + 1) * n_kv_heads * 64 * head_dim * element size < 2^31).
  * lsv_kv_pool_bytes: size of the buffer (0 if cfg is invalid). */
 size_t lsv_kv_pool_bytes(const lsv_model_config* cfg, int32_t n_pages);
 
@@ -239,15 +239,18 @@ int lsv_verify_paged(const lsv_model_config* cfg, const void* d_packed, void* d_
 /* The parts of an attention layer as calls of their own, for programs that run their own decoder
  * layers on the library's cache: rotary forms and scores that lsv_verify_block does not have, and
  * chunks of more than LSV_MAX_ROWS rows.  They read and write one layer of the paged cache
- * (layout above), so a cache that they fill serves lsv_verify_paged and the other way round; a
- * slab cache of `batch` sequences is a pool of batch * capacity / 64 pages under the identity
- * table (page_table[b * max_pages + p] = b * capacity / 64 + p).
+ * (layout above), of any size (the 2 GiB limit of a layer's K pool is the verify step's).  A cache
+ * that they fill serves lsv_verify_paged, and the other way round, where its keys were rotated as
+ * the verify step does: LSV_ROPE_HALF over the whole head, LSV_ROPE_PLAIN at cfg->rope_base,
+ * amplitude 1.  A slab cache of `batch` sequences is a pool of batch * capacity / 64 pages under the
+ * identity table (page_table[b * max_pages + p] = b * capacity / 64 + p).
  *
  * Rows are as for lsv_verify_block: sequence b owns rows d_row_offsets[b] ..
  * d_row_offsets[b+1]-1 of the row arrays, row i of its block sits at position d_seq_len[b] + i,
  * and d_seq_len is not modified.  Row arrays are [rows][heads][head_dim] in the model dtype, the
  * heads of a row adjacent and rows `stride` elements apart (so q, k and v may be slices of one
- * fused projection); rows at or past d_row_offsets[batch] are neither read nor written.
+ * fused projection).  The first offset need not be 0: rows before it, and those at or past
+ * d_row_offsets[batch], are neither read nor written.
  *
  * d_status of lsv_append_paged and lsv_attend_paged ([batch] int32 out, nullable): LSV_OK;
  * LSV_ERR_INVALID_ARG for a sequence whose row offsets decrease, fall behind an earlier offset,
@@ -339,6 +342,9 @@ int lsv_append_paged(const lsv_model_config* cfg, int32_t layer, void* d_kv_pool
  * A row that sees no key gets out = 0 and lse = -inf.  What a row does not see has no effect on
  * it, whatever the cache holds there (infinities and NaN included).  Keys whose page entry is
  * outside the pool read as zeros, as in lsv_verify_paged.
+ * The same call gives the same bits, but where a row's keys are cut follows from the lengths of all
+ * sequences and the host bounds: unlike in lsv_verify_block, a token alone, in a batch or in a block
+ * can get different roundings, and a choice between equal logits with them.
  * Scores, softmax statistics and sums are fp32; in bf16 the probabilities are rounded to bf16
  * (relative to a score within 2^8 of the largest so far) as the operand of the product with V.
  *   options (nullable: the plain causal score), all fields zero for a default:

@@ -15,7 +15,8 @@
 //  * merge kernels: join the sums of tiles whose pages were cut over workgroups.
 //
 // Pages go to LDS by direct loads, whole lines of 16 bytes a lane: fragments of 64 bytes loaded straight into
-// operands reach 4.4 to 5.1 TB/s, these 6.2 (64 ragged sequences, 1.08 GB: 246 -> 183 us).
+// operands reach 4.4 to 5.1 TB/s, these 6.2 (64 ragged sequences, 1.08 GB: 246 -> 183 us by this alone, 170 with what
+// followed).
 #include <math.h>
 
 #include "lsv_attn.h"
@@ -329,6 +330,8 @@ template <typename T> LSV_DEV void clean_fragment(u32x4_t& f) {
 // One pass over a chain's pages with the running maximum m and sum l of the softmax: for a step's scores s_j (in log2
 // units), m' = max(m, s_j), p_j = 2^(s_j - m'), l' = l 2^(m - m') + sum p_j and o' = o 2^(m - m') + sum p_j v_j; a row's
 // result is o / l and m + log2 l.  Parts of a chain join by the same rule, so its pages may be cut anywhere.
+// Exponentials are the hardware's 2^x, in fp32 too: off by 2^-22 of a probability, where the score that it comes from is off
+// by up to HD 2^-24 of its largest products.
 // Reading K and V bounds it, once each: a page meets every query vector of its tile.  Measured: 64 sequences of one
 // token behind 200 to 8000 positions, 1.08 GB in 170 us (6.3 TB/s; four waves a workgroup that took whole sequences:
 // 257); two of four tokens behind 100K to 131K, 0.95 GB in 150 us + 10 for the merge; one token behind 2047, 8.4 MB: 10.7 us,
@@ -349,7 +352,9 @@ template <int HD> struct Stream<bf16_t, HD> {
   LSV_DEV static f32x4_t score(u32x4_t k, u32x4_t q, f32x4_t s) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, k), __builtin_bit_cast(bf16x8_t, q), s, 0, 0, 0);
   }
-  // P^T as an operand: rounded to bf16, so that the product runs on the matrix cores
+  // P^T as an operand: rounded to bf16, so that the product runs on the matrix cores at their bf16 rate.  An output
+  // is off by up to 2^-8 of the mean |v| for it (1.2 to 1.4 times the error of rounding the output alone, over random
+  // values); l sums the probabilities as they were.
   struct P {
     bf16x8_t p[2];
   };
@@ -790,8 +795,8 @@ __global__ void __launch_bounds__(64 * kStreamWaves, 1) attend_stream_kernel(Att
 // of 64 keys, and O^T += V^T P^T.  A workgroup's four waves share a page's K and V in LDS, so that it is
 // loaded once for 128 query vectors; two workgroups a compute unit fill each other's waits.
 // The matrix cores and the exponentials bound it, and for long calls the power that both draw: 4096 rows behind
-// 4000, 64 heads: 755 us, 1.08 PFLOP/s, the matrix cores busy 54 % and the vector units 48 % of the cycles at a clock that
-// falls to 1.85 GHz (a plain product of 8192^3 reaches 1.19 PFLOP/s); 2047 rows behind 6001, 32 heads: 227 us.  At head
+// 4000, 64 heads: 759 us, 1.07 PFLOP/s, the matrix cores busy 54 % and the vector units 48 % of the cycles at a clock that
+// falls to 1.85 GHz (a plain product of 8192^3 reaches 1.19 PFLOP/s); 2047 rows behind 6001, 32 heads: 231 us.  At head
 // dimension 64 a score costs as many vector instructions for half the products: capped scores in a window of 1000,
 // four sequences of 700 to 1500 rows, 16 heads: 48 us, 0.34 PFLOP/s, the clock at 2.6 GHz.
 constexpr int kTileQ = 128;  // query vectors of a workgroup, 32 a wave
@@ -977,7 +982,7 @@ __global__ void __launch_bounds__(256, 2) attend_tile_kernel(AttendArgs a, Atten
         sum += sc[kb][r];
       }
     lrun += sum;
-    bf16x8_t pb8[2][2];  // the probabilities as an operand: rounded to bf16
+    bf16x8_t pb8[2][2];  // the probabilities as an operand: rounded to bf16, as in the stream kernel
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -1099,7 +1104,9 @@ __global__ void __launch_bounds__(256, 2) attend_tile_kernel(AttendArgs a, Atten
 }
 
 // ------------------------------------------------------------------ merge kernels
-// Bound by the chain of loads that finds a part and, at most, some 9 MB of sums: 5 to 10 us.
+// Bound by the chain of loads that finds a part, and by the sums: at most 1024 slots of 32 x HD (16.8 MB at 128) of the
+// stream kernel, 512 of 128 x HD (33.6 MB) of the tile kernel.  Two sequences of four tokens behind 100K to 131K: 8.7 MB in
+// 9.3 us; nothing to join: 4.2.
 // The stream kernel's chains: blockIdx.x + 1 is a share whose start lies inside a chain; the first such share
 // of a chain joins its parts.  blockIdx.y: the query vectors in lots of 1024 / HD, four dimensions a lane;
 // blockIdx.z: the kv head.

@@ -4,7 +4,8 @@
 // multiply-adds, so memory bounds them (or, for a few rows, the launch and its chain of loads).  A
 // thread keeps one unit of a head -- the same 16-byte piece, or pair of pieces, in every head -- of one row:
 // it forms that unit's cosines and sines once, in registers, and then walks the heads with four
-// loads in flight.  (A wave for every head, which formed them anew: 55 us where this takes 28.6.)
+// loads in flight.  (A wave for every head, which formed them anew: 55 us where this takes 27.7.)
+// Times are of a kernel in a captured graph; a call that the host waits for nowhere adds what its launch does.
 #include "lsv_attn.h"
 #include "lsv_ops.h"
 
@@ -13,7 +14,9 @@ namespace lsv {
 constexpr int kThreads = 256;
 constexpr int kPage = LSV_KV_PAGE;
 
-// amplitude * (cos, sin) of a pair at a position: the product in fp64, reduced to [-1, 1] half turns
+// amplitude * (cos, sin) of a pair at a position: the product in fp64, reduced to [-1, 1] half turns.  The reduced angle is
+// rounded to fp32, which moves a rotated element by 2^-23.3 of the pair at most, less than its sine's and its own
+// roundings to fp32 together (2^-22); sines in fp64 would be stored in no more bits.
 LSV_DEV float2 rope_turn(float amplitude, double half_turns, int pos) {
   const double t = (double)pos * half_turns;
   float sn, cs;
@@ -121,8 +124,8 @@ static bool aligned16(const void* p, int64_t stride, size_t es) {
 }
 
 // ------------------------------------------------------------------ rotation of a row array
-// A workgroup takes `group` rows and `lot` heads.  8191 rows of 40 heads of 128: 168 MB in 28.6 us, 5.9 TB/s (a copy of
-// 1 GiB moves 5.1); 32 rows: 3.6 us in a graph, the launch.
+// A workgroup takes `group` rows and `lot` heads.  8191 rows of 40 heads of 128: 168 MB in 27.7 us, 6.1 TB/s (a copy of
+// 1 GiB moves 5.1); 32 rows: 4.0 us by positions, the launch, 4.9 as 32 sequences by their lengths.
 template <typename T, bool VEC, bool HALF>
 __global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs rope, RowArgs rows, int group, int lot, const T* x,
                                                         int64_t xs, T* y, int64_t ys, int heads, int hd, bool copy) {
@@ -200,7 +203,7 @@ int launch_rope(const RopeArgs& rope, int dtype, int heads, int hd, const RowArg
 // ------------------------------------------------------------------ append
 // A workgroup takes the rows of one sequence that fall into one page (blockIdx.x counts these page
 // runs over the sequences) and one kv head with its query heads: up to 64 rows.  4095 rows of 64 + 8 + 8 heads: 168 MB in
-// 32.5 us, 5.2 TB/s; 32 sequences of one token: 5.9 us in a graph, bound by its chain of loads.  V goes through LDS:
+// 32.0 us, 5.2 TB/s; 32 sequences of one token: 6.1 us, bound by its chain of loads.  V goes through LDS:
 // rows come in along the head, the page wants them along the positions, eight permuted columns to
 // 16 or 32 bytes.  Its loads are the first, its stores the last.
 template <typename T, int HD, bool VEC, bool HALF>
