@@ -343,8 +343,9 @@ int lsv_append_paged(const lsv_model_config* cfg, int32_t layer, void* d_kv_pool
  * it, whatever the cache holds there (infinities and NaN included).  Keys whose page entry is
  * outside the pool read as zeros, as in lsv_verify_paged.
  * The same call gives the same bits, but where a row's keys are cut follows from the lengths of all
- * sequences and the host bounds: unlike in lsv_verify_block, a token alone, in a batch or in a block
- * can get different roundings, and a choice between equal logits with them.
+ * sequences, the host bounds and the key starts and prefixes of the rows beside it: unlike in
+ * lsv_verify_block, a token alone, in a batch or in a block can get different roundings, and a choice
+ * between equal logits with them.
  * Scores, softmax statistics and sums are fp32; in bf16 the probabilities are rounded to bf16
  * (relative to a score within 2^8 of the largest so far) as the operand of the product with V.
  *   options (nullable: the plain causal score), all fields zero for a default:

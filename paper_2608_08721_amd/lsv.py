@@ -71,7 +71,7 @@ class AttendOptions(ctypes.Structure):
     def __setattr__(self, name, value):
         if name.startswith("d_"):
             self.__dict__.pop(name, None)
-            if value is not None and not isinstance(value, int):
+            if hasattr(value, "data_ptr"):
                 self.__dict__[name] = value  # behind the field of that name, which holds the address
                 value = value.data_ptr()
         super().__setattr__(name, value)
@@ -208,8 +208,9 @@ def _holds(name, x, nbytes, dtype):
         _refuse(name, x, dtype, nbytes, "bytes")
 
 
-def _pool_bytes(cfg, n_pages):
-    return (2 * LSV_KV_PAGE * (2 if cfg.dtype == LSV_DTYPE_BF16 else 4) * cfg.n_layers * n_pages * cfg.n_kv_heads *
+def _pool_bytes(cfg, layer, n_pages):
+    """The layers up to that one, which is what a call on it can reach."""
+    return (2 * LSV_KV_PAGE * (2 if cfg.dtype == LSV_DTYPE_BF16 else 4) * (layer + 1) * n_pages * cfg.n_kv_heads *
             cfg.head_dim)
 
 
@@ -361,7 +362,8 @@ def lsv_apply_rope(rope, dtype, n_heads, head_dim, batch, seq_len, row_offsets, 
                    y_stride, stream=None):
     lib, t = load(), _TYPES.get(dtype)
     stream, seq_len, row_offsets, positions, x, y = _here(
-        stream, ("seq_len", seq_len, _I32, batch if positions is None else 0), ("row_offsets", row_offsets, _I32, batch + 1),
+        stream, ("seq_len", seq_len, *((_I32, batch) if positions is None else (None, ROWS))),
+        ("row_offsets", row_offsets, _I32, batch + 1),
         ("positions", positions, _I32, max_rows if row_offsets is None else 0), ("x", x, t, ROWS), ("y", y, t, ROWS))
     _check(lib.lsv_apply_rope(ctypes.byref(rope), dtype, n_heads, head_dim, batch, seq_len, row_offsets, positions,
                               max_rows, x, x_stride, y, y_stride, stream))
@@ -375,7 +377,7 @@ def lsv_append_paged(cfg, layer, kv_pool, n_pages, page_table, max_pages, batch,
         stream, ("kv_pool", kv_pool, None, ROWS), ("page_table", page_table, _I32, batch * max_pages),
         ("seq_len", seq_len, _I32, batch), ("row_offsets", row_offsets, _I32, batch + 1), ("positions", positions, _I32, 0),
         ("q", q, t, ROWS), ("q_out", q_out, t, ROWS), ("k", k, t, ROWS), ("v", v, t, ROWS), ("status", status, _I32, batch))
-    _holds("kv_pool", pool, _pool_bytes(cfg, n_pages), t)
+    _holds("kv_pool", pool, _pool_bytes(cfg, layer, n_pages), t)
     _check(lib.lsv_append_paged(ctypes.byref(cfg), layer, kv_pool, n_pages, page_table, max_pages, batch, seq_len,
                                 row_offsets, positions, max_rows, max_ctx,
                                 ctypes.byref(rope) if rope is not None else None, q, q_stride, q_out, q_out_stride, k,
@@ -397,7 +399,7 @@ def lsv_attend_paged(cfg, layer, kv_pool, n_pages, page_table, max_pages, batch,
         ("out", out, t, ROWS), ("lse", lse, _F32, 0), ("status", status, _I32, batch), ("ws", ws, None, ROWS),
         ("d_slopes", kept.get("d_slopes"), _F32, cfg.n_q_heads), ("d_key_start", kept.get("d_key_start"), _I32, 0),
         ("d_prefix_len", kept.get("d_prefix_len"), _I32, batch))
-    _holds("kv_pool", pool, _pool_bytes(cfg, n_pages), t)
+    _holds("kv_pool", pool, _pool_bytes(cfg, layer, n_pages), t)
     _holds("ws", space, ws_bytes, None)
     _check(lib.lsv_attend_paged(ctypes.byref(cfg), layer, kv_pool, n_pages, page_table, max_pages, batch, seq_len,
                                 row_offsets, max_rows, max_rows_per_seq, max_ctx,

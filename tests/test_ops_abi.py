@@ -187,7 +187,7 @@ def test_struct_sizes():
 
 def test_tensors_of_another_type_or_length_are_refused(lib, monkeypatch):  # noqa: F811
     """The binding's own checks, on tensors that say they lie on the current GPU: none of these calls reaches the library,
-    whose refusals (a layer out of range, no rows) show that the right tensors pass."""
+    whose refusals (no positions, no rows) show that the right tensors pass."""
     torch = pytest.importorskip("torch")
 
     class Here(torch.Tensor):
@@ -216,25 +216,27 @@ def test_tensors_of_another_type_or_length_are_refused(lib, monkeypatch):  # noq
                            256, S)
 
     def append(a):
-        lsv.lsv_append_paged(cfg, 9, a["pool"], n_pages, a["table"], P, B, a["seq"], a["off"], a["pos"], 8, 256, rope(),
+        lsv.lsv_append_paged(cfg, a.get("layer", 1), a["pool"], n_pages, a["table"], P, B, a["seq"], a["off"], a["pos"], 8, 0, rope(),
                              a["rows"], 256, a["rows"], 256, a["rows"], 256, a["rows"], 256, a["status"], S)
 
     def attend(a):
         o = lsv.AttendOptions(d_slopes=a["d_slopes"])
         o.d_key_start, o.d_prefix_len = a["d_key_start"], a["d_prefix_len"]
-        lsv.lsv_attend_paged(cfg, 9, a["pool"], n_pages, a["table"], P, B, a["seq"], a["off"], 8, 4, 256, o, a["rows"], 256,
+        lsv.lsv_attend_paged(cfg, a.get("layer", 1), a["pool"], n_pages, a["table"], P, B, a["seq"], a["off"], 8, 4, 0, o, a["rows"], 256,
                              a["rows"], 256, a["lse"], a["status"], a["ws"], 1 << 20, S)
 
-    for call, names, last in ((rotate, "off pos rows", "max_rows"), (append, "pool table seq off pos rows status", "layer 9"),
-                              (attend, "pool table seq off rows lse status ws d_slopes d_key_start d_prefix_len", "layer 9")):
+    for call, names, last in ((rotate, "off pos rows", "max_rows"), (append, "pool table seq off pos rows status", "max_ctx"),
+                              (attend, "pool table seq off rows lse status ws d_slopes d_key_start d_prefix_len", "max_ctx")):
         assert last in expect(BAD, call, right)
         assert last in expect(BAD, call, dict(right, pool=on(pool.nbytes, t=u8)))
+        assert last in expect(BAD, call, dict(right, pool=on(pool.nbytes // 2, t=u8), layer=0))  # a pool of its own layer
         for name in names.split():
             for x in wrong[name]:
                 assert "need a" in expect(BAD, call, dict(right, **{name: x})), (call, name, x.dtype, x.shape)
     # lengths in place of positions, and rows of the other type
     assert "need a" in expect(BAD, rotate, dict(right, pos=None, seq=on(B, t=torch.int64)))
     assert "need a" in expect(BAD, rotate, right, lsv.LSV_DTYPE_BF16)
+    assert "max_rows" in expect(BAD, rotate, dict(right, seq=on(1, t=torch.int64)))  # with positions not read
 
 
 def test_options_keep_their_tensors():
@@ -251,6 +253,8 @@ def test_options_keep_their_tensors():
     o.d_slopes = at  # an address from now on
     gc.collect()
     assert seen() is None and o.d_slopes == at
+    o.d_slopes = ctypes.c_void_p(at)
+    assert o.d_slopes == at
     o.d_slopes = None
     assert o.d_slopes is None
 
