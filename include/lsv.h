@@ -301,7 +301,7 @@ int lsv_rope_init(lsv_rope* rope, int32_t layout, int32_t rot_dim, double base, 
  *                   before the first offset and from the last on stay as they were, and all of them
  *                   unless 0 <= first <= last <= max_rows (with d_positions no other is read).
  *                   Without d_positions so do the rows of a sequence that lsv_append_paged would
- *                   refuse with LSV_ERR_INVALID_ARG, or whose positions pass 2^31 - 1
+ *                   refuse with LSV_ERR_INVALID_ARG, or whose positions reach 2^31 - 1
  *   d_seq_len       [batch] int32, read only without d_positions (else nullable)
  *   max_rows        host bound on the rows, 1..LSV_MAX_CHUNK_ROWS
  *   d_x, d_y        row arrays; d_y == d_x with equal strides rotates in place (other overlaps

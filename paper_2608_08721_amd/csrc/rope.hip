@@ -5,7 +5,7 @@
 // thread keeps one unit of a head -- the same 16-byte piece, or pair of pieces, in every head -- of one row:
 // it forms that unit's cosines and sines once, in registers, and then walks the heads with four
 // loads in flight.  (A wave for every head, which formed them anew: 55 us where this takes 27.7.)
-// Times are of a kernel in a captured graph; a call that the host waits for nowhere adds what its launch does.
+// Times are the kernel's, in a captured graph.
 #include "lsv_attn.h"
 #include "lsv_ops.h"
 
@@ -52,8 +52,8 @@ __host__ __device__ inline Units units_of(int layout, int rot, int hd, int n, bo
 }
 
 // Rotate `nrow` rows of `heads` heads: from(r, h) and to(r, h) are head h of row r, pos(r, p) sets the row's
-// position, false: the row stays as it is.  Threads take (unit, row, head) with the unit fastest.  A thread owns both elements of its
-// pairs, so that rotating in place is safe; the unrotated tail goes over only where `copy` says so.
+// position, false: the row stays as it is.  Threads take (unit, row, head) with the unit fastest.  A thread owns
+// both elements of its pairs, so that rotating in place is safe; the unrotated tail goes over only where `copy` says so.
 template <typename T, bool VEC, bool HALF, typename From, typename To, typename Pos>
 LSV_DEV void rotate_rows(const RopeArgs& rope, int nrow, int heads, int hd, bool copy, From from, To to, Pos pos) {
   constexpr int N = VEC ? 16 / (int)sizeof(T) : 1;   // elements of a piece

@@ -186,3 +186,23 @@ def test_one_graph_under_changing_lengths():
             assert torch.equal(c.out, want) and torch.equal(c.lse, lse)
         assert (want[sum(rows):] == 7.0).all() and (want[:sum(rows), :c.W] != 7.0).any() == (sum(rows) > 0)
     assert len({(pps != ALL, parts > 1) for pps, _, parts in seen}) == 3, seen
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("C,rows", [([900, 30], [1, 2]), ([300, 0], [60, 33])])
+def test_offsets_that_begin_behind_zero(dtype, C, rows):
+    """The same rows three places further on: the same bits there, and the rows before them as they were."""
+    c = Case(90, 8, 2, 128, dtype, C, rows)
+    c.call()
+    c.check()
+    M, out, lse = c.s.M, c.out[:c.s.M].clone(), c.lse[:c.s.M].clone()
+    c.q[3:] = c.q[:M].clone()
+    c.q[:3] = float("nan")
+    c.dev = i32(C), i32(np.asarray(c.s.off) + 3)
+    c.out.fill_(7.0)
+    c.lse.fill_(7.0)
+    c.call()
+    torch.cuda.synchronize()
+    assert c.s.status.tolist() == [0, 0]
+    assert torch.equal(c.out[3:], out) and torch.equal(c.lse[3:], lse)
+    assert (c.out[:3] == 7.0).all() and (c.lse[:3] == 7.0).all()

@@ -299,3 +299,23 @@ def test_rope_leaves_refused_sequences_alone():
         lsv.lsv_apply_rope(r, lsv.LSV_DTYPE_F32, 1, 64, 3, i32(C), i32(off), None, 12, y, 64, y, 64)
         torch.cuda.synchronize()
         assert torch.equal(y, want), (C, off)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_append_takes_the_rows_that_the_offsets_name(dtype):
+    """Offsets that begin behind 0: the pages and queries of a call without the rows before them."""
+    rng = np.random.default_rng(13)
+    C, rows, first = [61, 0], [70, 3], 5
+    s = Layer(rng, 4, 2, 64, dtype, C, rows)
+    x = torch.tensor(rng.normal(size=(s.M + first, 8 * 64)), device="cuda").to(s.t)
+    r, got = make_rope(64), []
+    for at in (0, first):
+        s.pool.fill_(float("nan"))
+        q = torch.full((s.M + first, 256), 7.0, dtype=s.t, device="cuda")
+        rows_ = x[first - at:]
+        lsv.lsv_append_paged(s.cfg, 0, s.pool, s.n_pages, s.table, s.max_pages, 2, i32(C), i32(s.off + at), None, s.M + at,
+                             s.max_ctx, r, rows_, 512, q, 256, rows_[:, 256:], 512, rows_[:, 384:], 512, s.status)
+        torch.cuda.synchronize()
+        assert s.status.tolist() == [0, 0] and (q[:at] == 7.0).all()
+        got.append((q[at:at + s.M].clone(), s.pool.clone().view(torch.uint8)))
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
